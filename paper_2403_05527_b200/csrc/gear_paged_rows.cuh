@@ -77,6 +77,13 @@ __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t h
 template <class T> struct IsHalf { static constexpr bool value = false; };
 template <> struct IsHalf<__half> { static constexpr bool value = true; };
 
+// Probabilities and their sums are kept beside a base: 2^-kSpare of the largest of them when it was last moved, and moved again once one
+// passes 2^(kSpare + 8).  An operand of fp16 is subnormal below 2^-14, zero below 2^-25, and has room up to 2^16: with the seven powers that the
+// lag leaves spare, the tail behind a token that takes nearly all of the sum keeps its bits down to 2^-21 of it, and what it has at all down to
+// 2^-32.  (With none, tails 2^-20 to 2^-26 below such tokens were off by 1.5 to 7 times what their roundings allow: the sum takes them unrounded.)
+template <class T> constexpr float kSpare = IsHalf<T>::value ? 7.f : 0.f;
+template <class T> constexpr float kRise = kSpare<T> + 8.f;
+
 // Four packed pairs of codes 4 bits wide from a word, x = (nibble 0, nibble 4), (1, 5), (2, 6), (3, 7): the code is put below a constant whose
 // last place is one, which is then subtracted
 template <class T> struct Biases {
@@ -428,7 +435,7 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
             }
           }
         }
-        // ---- probabilities beside a maximum that lags by up to 2^8
+        // ---- probabilities beside a base that lags by up to 2^8
         bool rises = false;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
@@ -445,7 +452,7 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
                 }
                 top = fmaxf(top, z[h][n][x]);
               }
-            rises = rises || top * a.scale_log2 > m[n][e] + 8.f;
+            rises = rises || top * a.scale_log2 > m[n][e] + kRise<T>;
           }
         if (__any_sync(0xffffffffu, rises)) {
 #pragma unroll
@@ -457,7 +464,7 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
               for (int h = 0; h < SUB; ++h) top = fmaxf(top, fmaxf(z[h][n][e], z[h][n][e + 2]));
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-              top = fmaxf(m[n][e], top * a.scale_log2);
+              top = fmaxf(m[n][e], fmaf(top, a.scale_log2, -kSpare<T>));
               const float keep = exp2_fast(m[n][e] - top);
               m[n][e] = top;
               l[n][e] *= keep;

@@ -6,8 +6,8 @@
 // that a short chunk of grouped heads fills them; a tile takes whole new rows) against blocks of 128 tokens.  Its two tiles take turns: while one tile's
 // probabilities are computed the tensor cores work for the other.  Per tile and block S = Q K^T (operands in shared memory) lands in
 // tensor memory, one thread per row turns it into probabilities, which go back over the scores as the A operand of O += P V.  O
-// stays in tensor memory and is scaled only when a maximum rises by more than 2^8 (sums and outputs are kept beside that lagging
-// maximum).  Tensor memory: S0 | S1 | O0 | O1, 128 columns each.
+// stays in tensor memory and is scaled only when a maximum rises by more than 2^8 (sums and outputs are kept beside a lagging
+// base, kSpare in gear_paged_rows.cuh).  Tensor memory: S0 | S1 | O0 | O1, 128 columns each.
 //
 // Blocks of all units, one after the other, are cut into equal ranges, one per SM; units that lie in several ranges leave partial
 // results for paged_tile_join_kernel.  paged_tile_plan_kernel sums the units' blocks beforehand.

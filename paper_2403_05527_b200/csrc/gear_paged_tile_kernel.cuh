@@ -187,8 +187,8 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
             }
             if (kHeld < 4) tmem_ld32_begin(s[0], tS);
             const float z = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-            if (__any_sync(0xffffffffu, z > m + 8.f)) {
-              const float next = fmaxf(m, z), keep = next == -INFINITY ? 1.f : exp2_fast(m - next);
+            if (__any_sync(0xffffffffu, z > m + kRise<T>)) {      // m: the base (kSpare)
+              const float next = fmaxf(m, z - kSpare<T>), keep = next == -INFINITY ? 1.f : exp2_fast(m - next);
               m = next;
               l *= keep;
               if (j > 0) {                                     // O of the blocks so far; the first product writes over what is there
