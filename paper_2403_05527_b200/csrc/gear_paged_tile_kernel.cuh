@@ -187,7 +187,9 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
             }
             if (kHeld < 4) tmem_ld32_begin(s[0], tS);
             const float z = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-            if (__any_sync(0xffffffffu, z > m + kRise<T>)) {      // m: the base (kSpare)
+            // m: the base (kSpare).  Only rows of the unit have a say: the others hold the next sequences' rows, nobody's, or what shared
+            // memory held before
+            if (__any_sync(0xffffffffu, mine && z > m + kRise<T>)) {
               const float next = fmaxf(m, z - kSpare<T>), keep = next == -INFINITY ? 1.f : exp2_fast(m - next);
               m = next;
               l *= keep;
