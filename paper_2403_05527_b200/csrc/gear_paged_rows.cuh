@@ -28,7 +28,7 @@ namespace gear {
 
 // (sequence, kv head) units have parts of their own where CTAs are at least kOwnShare times as many (and the sequences kOwnSeqs at most)
 constexpr int kOwnShare = 4, kOwnSeqs = 96;
-constexpr int kFineTokens = 1024;            // tokens that a table has room for, up to which codes get probabilities in two parts
+constexpr int kFineTokens = 1024;            // tokens that a sequence's rows see, up to which codes get probabilities in two parts
 constexpr int kStep = 16;                    // tokens of a product: every page holds whole ones
 // products of a step: with codes two, which share what a step costs apart from its tokens (12 contexts of 32768 in 4 bits: 612 instructions
 // per 16 tokens and 171 us with one); rows as they are wait for memory either way and would fill shared memory
@@ -148,11 +148,11 @@ template <int BITS, int D, int NQ, int W> struct RowsRing {
   static constexpr int kBytes = kQuery + NQ * 8 * kQPitch;
 };
 
-// W warps, NQ blocks of 8 query rows.  FINE: probabilities as a rounded part and the rest rounded (16 bits and more between them).  Rounded
+// W warps, NQ blocks of 8 query rows.  Fine: probabilities as a rounded part and the rest rounded (16 bits and more between them).  Rounded
 // once, few tokens that share most of the sum leave outputs half as far off again as their own rounding does.  Rows as they are have the
-// time for it (131 -> 133 us); with codes it costs 8 % (12 contexts of 32768 in 4 bits 134 -> 147 us), and only caches of short
-// contexts get it.
-template <class T, int BITS, int D, int NQ, int W, int MINB, bool FINE>
+// time for it (131 -> 133 us); with codes it costs 8 % (12 contexts of 32768 in 4 bits 134 -> 147 us), and only sequences whose rows see
+// at most kFineTokens tokens get it.
+template <class T, int BITS, int D, int NQ, int W, int MINB>
 __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs a, int group_shift, int least, int own_units) {
   using S = RowsRing<BITS, D, NQ, W>;
   const PagedArgs& c = a.c;
@@ -370,10 +370,10 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
         phases ^= 1u << stage;
         if (!ok) there = 0;
       }
-      // The arithmetic of a step, made twice: most steps have nothing to mask (selected by a condition in one piece of code, masks were
-      // computed in every step)
+      // The arithmetic of a step, made with and without masks, as most steps have nothing to mask (selected by a condition in one piece of
+      // code, masks were computed in every step), and fine or not
       auto step = [&](auto kind) {
-        constexpr bool kWhole = decltype(kind)::value, kFine = FINE;
+        constexpr bool kWhole = decltype(kind)::value & 1, kFine = decltype(kind)::value & 2;
         // ---- scores: z[..][n][0..1] token r, z[..][n][2..3] token r + 8, rows 2 i4 and 2 i4 + 1 of block n
         float z[SUB][NQ][4];
 #pragma unroll
@@ -569,8 +569,12 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
           }
         }
       };
-      if (there == (1u << SUB) - 1 && t0 >= lo_max && t0 + kSpan <= hi_min) step(std::true_type());
-      else step(std::false_type());
+      const bool whole = there == (1u << SUB) - 1 && t0 >= lo_max && t0 + kSpan <= hi_min;
+      if (BITS == 16 || u.hi - u.lo <= kFineTokens) {
+        if (whole) step(std::integral_constant<int, 3>()); else step(std::integral_constant<int, 2>());
+      } else if constexpr (BITS != 16) {
+        if (whole) step(std::integral_constant<int, 1>()); else step(std::integral_constant<int, 0>());
+      }
       // everything of the step has been used: the stage may be written again
       __syncwarp();
       request(k + NS, stage);
@@ -689,13 +693,13 @@ constexpr int kRowsMaxCtas = 148 * 4;
 // 64 heads x 500 12.0 -> 10.0; one head x 256 6.7 -> 7.6, x 8000 11.4 -> 12.8)
 constexpr int kRowsLeastTokens = 256, kRowsSeveral = 8;
 
-template <class T, int BITS, int D, int NQ, int W, int MINB, bool FINE>
+template <class T, int BITS, int D, int NQ, int W, int MINB>
 cudaError_t launch_rows_t(const PagedAttnArgs& a, int group, cudaStream_t st) {
   constexpr int kBytes = RowsRing<BITS, D, NQ, W>::kBytes;
   int shift = 0, sms = 0;
   while ((1 << shift) < group) ++shift;
   static KernelReady ready;
-  const cudaError_t e = ready.on_this_device(paged_rows_kernel<T, BITS, D, NQ, W, MINB, FINE>, kBytes, &sms);
+  const cudaError_t e = ready.on_this_device(paged_rows_kernel<T, BITS, D, NQ, W, MINB>, kBytes, &sms);
   if (e != cudaSuccess) return e;
   // no more CTAs than the longest contexts that the table has room for could use
   constexpr int kSpan = kStep * kStepParts<BITS>;
@@ -705,24 +709,18 @@ cudaError_t launch_rows_t(const PagedAttnArgs& a, int group, cudaStream_t st) {
   const long long most = units * ((long long)a.c.table_stride * a.c.page_size / kSpan + 2);
   const long long ctas = (most + least - 1) / least + own_units;
   count_launches(1);
-  return launch_dependent(paged_rows_kernel<T, BITS, D, NQ, W, MINB, FINE>, dim3((unsigned)std::min(ctas, room)), W * 32, kBytes, st, a, shift, least,
+  return launch_dependent(paged_rows_kernel<T, BITS, D, NQ, W, MINB>, dim3((unsigned)std::min(ctas, room)), W * 32, kBytes, st, a, shift, least,
                           own_units);
 }
-template <class T, int BITS, int D, bool FINE>
-cudaError_t launch_rows_f(const PagedAttnArgs& a, int group, cudaStream_t st) {
+template <class T, int BITS, int D>
+cudaError_t launch_rows_d(const PagedAttnArgs& a, int group, cudaStream_t st) {
   constexpr int W = BITS == 16 && D == 128 ? 4 : BITS == 8 && D == 128 ? 6 : 8;    // what two CTAs have room for
   // Few units of 16-bit rows: eight warps in one CTA per SM, whose parts are half as many (one head x 256 tokens 7.4 -> 6.7 us,
   // 8 heads x 32000 31.6 -> 30.0; 32 heads x 4000 16.6 -> 17.2)
   if constexpr (BITS == 16 && D == 128)
     if (a.max_rows * a.share <= 8 && (long long)a.c.n_seqs * a.c.heads * kOwnShare <= 148 && a.c.n_seqs <= kOwnSeqs)
-      return launch_rows_t<T, BITS, D, 1, 8, 1, FINE>(a, group, st);
-  return a.max_rows * a.share <= 8 ? launch_rows_t<T, BITS, D, 1, W, 2, FINE>(a, group, st) : launch_rows_t<T, BITS, D, 2, 4, 2, FINE>(a, group, st);
-}
-template <class T, int BITS, int D>
-cudaError_t launch_rows_d(const PagedAttnArgs& a, int group, cudaStream_t st) {
-  if constexpr (BITS != 16)
-    if ((long long)a.c.table_stride * a.c.page_size > kFineTokens) return launch_rows_f<T, BITS, D, false>(a, group, st);
-  return launch_rows_f<T, BITS, D, true>(a, group, st);
+      return launch_rows_t<T, BITS, D, 1, 8, 1>(a, group, st);
+  return a.max_rows * a.share <= 8 ? launch_rows_t<T, BITS, D, 1, W, 2>(a, group, st) : launch_rows_t<T, BITS, D, 2, 4, 2>(a, group, st);
 }
 template <int BITS>
 cudaError_t launch_paged_rows_bits(const PagedAttnArgs& a, int dtype, int group, cudaStream_t st) {
