@@ -266,7 +266,10 @@ def _pages(t, name, token_bytes, n_kv_heads, page_size):
         raise ValueError(f"{name}: a page must be contiguous and hold {page} bytes")
     if t.dtype not in (torch.uint8, torch.float16, torch.bfloat16):
         raise ValueError(f"{name}: dtype {t.dtype}")
-    return t.shape[0], t.stride(0) * t.element_size() if t.shape[0] > 1 else page
+    distance = t.stride(0) * t.element_size() if t.shape[0] > 1 else page
+    if distance < page:                            # an expanded pool: fewer pages than it counts
+        raise ValueError(f"{name}: pages must not overlap")
+    return t.shape[0], distance
 
 
 def make_paged(k_pages, v_pages, page_table, lengths, dtype, page_size, n_kv_heads, head_dim=128, bits=16, group=0,
