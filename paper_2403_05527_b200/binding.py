@@ -296,6 +296,8 @@ def make_paged(k_pages, v_pages, page_table, lengths, dtype, page_size, n_kv_hea
     for name, t, dims in (("page_table", page_table, 2), ("lengths", lengths, 1)):
         if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.shape[0] != lengths.shape[0]:
             raise ValueError(f"{name} must be contiguous int32 with a row per sequence")
+    if bits == 16 and any(t.dtype not in (dtype, torch.uint8) for t in (k_pages, v_pages)):
+        raise ValueError(f"rows as they are need pools of {dtype} or of bytes")
     tensors = [t for t in (k_pages, v_pages, k_params, v_params, page_table, lengths) if t is not None]
     if any(t.device != k_pages.device for t in tensors):
         raise ValueError("pools, page_table and lengths must be on one device")

@@ -48,3 +48,14 @@ def test_pools_of_fewer_pages_than_they_count_are_refused(side):
     one = _on_device(1, HEADS, PAGE, D // 64, 2).expand(PAGES, HEADS, PAGE, D // 64, 2)
     with pytest.raises(ValueError):
         _make(*codes, bits=8, group=64, k_params=one, v_params=one)
+
+
+def test_pools_of_another_type_are_refused():
+    """Rows as they are in a pool of the other type of 16 bits would be read as numbers that they are not.  Bytes are taken for either."""
+    k, v = (_on_device(PAGES, HEADS, PAGE, D, dtype=torch.bfloat16) for _ in range(2))
+    assert _make(k, v, dtype=torch.bfloat16).struct.dtype == G.GEAR_BF16
+    raw = [_on_device(PAGES, HEADS, PAGE, D * 2, dtype=torch.uint8) for _ in range(2)]
+    assert _make(*raw, dtype=torch.bfloat16).struct.dtype == G.GEAR_BF16
+    for pair in ((k, v), (k, raw[1]), (raw[0], v)):
+        with pytest.raises(ValueError):
+            _make(*pair, dtype=torch.float16)
