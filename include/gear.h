@@ -393,6 +393,9 @@ gear_status gear_fp16_attn_static_status(int32_t* code);
  * GEAR_ERR_TIMEOUT and returns.  So do, behind their last blocks, the kernels that quantize a prompt whose
  * residual is not kept.  Nothing faults, traps or hangs. */
 gear_status gear_test_dead_wait(gear_cache* cache, int32_t on);
+/* The same for gear_paged_attn, for the whole process: while `which` is 1, the first warp of every CTA of the kernel of few rows
+ * waits once, behind its first requests, on a barrier that nothing completes.  0: off. */
+gear_status gear_paged_test_dead_wait(int32_t which);
 
 const char* gear_strerror(gear_status s);
 

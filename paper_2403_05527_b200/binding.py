@@ -100,6 +100,7 @@ _SIGNATURES = {
                                     C.c_size_t, C.c_void_p]),
     "gear_paged_attn": (C.c_int32, [C.POINTER(GearPagedCache), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                     C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "gear_paged_test_dead_wait": (C.c_int32, [C.c_int32]),
     "gear_strerror": (C.c_char_p, [C.c_int32]),
     "gear_kernel_launches": (C.c_uint64, []),
 }
@@ -423,6 +424,10 @@ def gear_paged_attn(cache, q, out, row_start, scratch, max_rows: int, lse=None, 
     return _check(lib().gear_paged_attn(cache.ref, qp, qs, _dense(out), lp, _int32(row_start, cache.n_seqs + 1, "row_start"), n_rows,
                                         max_rows, heads, 1 if causal else 0, window, softmax_scale, _dense(scratch), scratch.nbytes,
                                         _stream(stream)), "gear_paged_attn")
+
+
+def gear_paged_test_dead_wait(which: int) -> None:
+    _check(lib().gear_paged_test_dead_wait(which), "gear_paged_test_dead_wait")
 
 
 def gear_free(cache) -> None:

@@ -402,6 +402,8 @@ static gear_status check_stride(int64_t stride, int64_t width, long long* bytes)
   return GEAR_OK;
 }
 
+static std::atomic<int> test_dead_wait{0};
+
 static gear_status launched(cudaError_t e) {
   if (e == cudaSuccess) return GEAR_OK;
   cudaGetLastError();
@@ -454,6 +456,12 @@ extern "C" gear_status gear_paged_read(const gear_paged_cache* cache, void* K, v
                                            : read_bits<__nv_bfloat16>(a, cache->bits, K, V, first, n, cache->group, st));
 }
 
+extern "C" gear_status gear_paged_test_dead_wait(int32_t which) {
+  if (which < 0 || which > 1) return GEAR_ERR_ARG;
+  test_dead_wait.store(which, std::memory_order_relaxed);
+  return GEAR_OK;
+}
+
 extern "C" size_t gear_paged_scratch_bytes(const gear_paged_cache* cache, int64_t n_rows, int32_t n_q_heads) {
   if (!cache || cache->n_seqs < 1 || cache->n_kv_heads < 1 || n_rows < 0 || n_q_heads < 1) return GEAR_PAGED_SCRATCH_MIN;
   return paged_attn_scratch(n_rows, (n_q_heads + cache->n_kv_heads - 1) / cache->n_kv_heads, cache->n_seqs);
@@ -480,5 +488,6 @@ extern "C" gear_status gear_paged_attn(const gear_paged_cache* cache, const void
   a.max_rows = (int)std::min<int64_t>(max_rows, n_rows);
   a.causal = causal != 0; a.window = window;
   a.scale_log2 = sc * 1.4426950408889634f;
+  a.test_dead_wait = test_dead_wait.load(std::memory_order_relaxed);
   return launched(launch_paged_attn(a, cache->bits, cache->dtype, cache->group, scratch, (cudaStream_t)stream));
 }

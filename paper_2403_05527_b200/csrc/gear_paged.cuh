@@ -41,6 +41,7 @@ struct PagedAttnArgs {
   int unit_cap, tile_ctas;
   int tile_new;                 // new rows of a tile: 128 / share
   void* shared_units;           // [tile_ctas] TileShared
+  int test_dead_wait;           // test only: the warp that waits on a barrier that nothing completes (gear_paged_test_dead_wait)
 };
 
 // What a kernel needs to be told once per device before it is launched there: the shared memory it takes beyond the default.  Calls from
@@ -68,6 +69,7 @@ class KernelReady {
 __device__ __forceinline__ unsigned char* pages_of(const PagedArgs& c, int side) { return side == 0 ? c.pages[0] : c.pages[1]; }
 __device__ __forceinline__ unsigned char* params_of(const PagedArgs& c, int side) { return side == 0 ? c.params[0] : c.params[1]; }
 
+constexpr int kTestSpinLimit = 64;             // polls, of 20 us at most, of a wait under gear_paged_test_dead_wait
 constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ void paged_bad(const PagedArgs& c) { atomicExch(c.status, GEAR_ERR_STATE); }

@@ -8,7 +8,7 @@
 // its own in shared memory by bulk copies (a lane each for keys, values and their parameters), several steps ahead; the warps of a CTA
 // take turns.  (With the next step's loads held in registers instead, 16-bit rows waited for memory, 64 ragged contexts up to 8192 168 us,
 // now 133, 87 % of the copy bandwidth; and codes spent 616 instructions per 16 tokens, half of them on addresses, 12 contexts of 32768 in 4
-// bits 161 us, now 428 and 127, bound by the issue of instructions and by their latency at 16 warps per SM.)
+// bits 161 us, now 428 and 129, bound by the issue of instructions and by their latency at 16 warps per SM.)
 //
 // Work: where there are few (sequence, kv head) units for the CTAs, each is cut evenly into parts of its own, a CTA each; else the steps of
 // all units, one after the other, are cut into equal ranges, one per CTA.  (Ranges that begin in one unit and end in the next cost a
@@ -167,17 +167,21 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
   unsigned char* qs = smem + S::kQuery;
   float* os = reinterpret_cast<float*>(smem);
   __shared__ float ms[W][kRows], ls[W][kRows];
-  __shared__ uint64_t full[W][NS];
+  __shared__ uint64_t full[W][NS], dead;
   __shared__ long long scan[W + 1];
   __shared__ long long start_at[1];
   __shared__ int start_seq, last_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, i4 = lane & 3;
   unsigned char* ring = smem + warp * NS * S::kStage;
   if (lane < NS) bar_init(&full[warp][lane]);
+  if (tid == 0) bar_init(&dead);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  uint32_t phases = 0;                                       // bit s: phase of stage s
+  // Bit s: phase of stage s; bit 8 + stage * SUB + part: there is data, or on its way; bit 31: a wait gave up, go on without data (every loop
+  // still ends).  From then on the others stay those of the copies in flight.  (In a register each: 12 contexts of 32768 in 4 bits 132 us, now 129.)
+  uint32_t ring_state = 0;
+  constexpr uint32_t kGaveUp = 1u << 31;
+  auto data_of = [&](int stage) { return ring_state >> (8 + stage * SUB) & ((1u << SUB) - 1); };
   const Biases<T> biases;
-  bool ok = true;                                            // a wait gave up: go on without data, every loop still ends
   after_previous();
 
   // ---- where this CTA's range begins.  f counts steps of all units, or, where units have parts of their own, those.
@@ -312,10 +316,10 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
     unsigned char* place = ring + sub_mine * S::kPart + (params ? 2 * S::kCodes + side * S::kParams : side * S::kCodes);
     const uint32_t part_bytes = 2 * kStep * (S::kRowBytes + (BITS == 16 ? 0 : c.param_row_bytes));
     int pages = 0;
-    uint32_t have = 0;                                       // bit stage * SUB + part: there is data
+    ring_state &= kGaveUp | 0xffu;
     // step k of this warp
     auto request = [&](int k, int stage) {
-      if (k >= steps_mine) return;
+      if (k >= steps_mine || (ring_state & kGaveUp)) return;
       if (k % kLook == 0) {
         const int mine = k + lane / SUB, t = u.first + (st0 + warp + mine * W) * kSpan + lane % SUB * kStep;
         pages = -1;
@@ -325,9 +329,9 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
         }
       }
       const int page = __shfl_sync(0xffffffffu, pages, k % kLook * SUB + (sub_mine & (SUB - 1)));
-      const uint32_t good = __ballot_sync(0xffffffffu, page >= 0 && ok && lane < 4 * SUB);    // bits 0 and 4
+      const uint32_t good = __ballot_sync(0xffffffffu, page >= 0 && lane < 4 * SUB);    // bits 0 and 4
       const uint32_t bits = (good & 1u) | (SUB == 2 ? good >> 3 & 2u : 0u);
-      have = (have & ~(((1u << SUB) - 1) << stage * SUB)) | bits << stage * SUB;
+      ring_state = (ring_state & ~(((1u << SUB) - 1) << (8 + stage * SUB))) | bits << (8 + stage * SUB);
       if (bits == 0) return;
       if (lane == 0) bar_expect(&full[warp][stage], part_bytes * __popc(bits));
       __syncwarp();
@@ -361,14 +365,18 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
         for (int x = 0; x < D / 32; ++x) qf[n][BITS == 16 ? x : 0] = query(n, x / (kKeyChannels / 8), x % (kKeyChannels / 8));
     }
 
+    if (a.test_dead_wait && warp == 0 && !bar_wait(&dead, 0, kTestSpinLimit)) ring_state |= kGaveUp;
     int stage = 0;
     for (int k = 0; k < steps_mine; ++k) {
       const int t0 = u.first + (st0 + warp + k * W) * kSpan;
-      uint32_t there = have >> stage * SUB & ((1u << SUB) - 1);
+      uint32_t there = data_of(stage);
       if (there) {
-        ok = __all_sync(0xffffffffu, ok && bar_wait(&full[warp][stage], phases >> stage & 1u));
-        phases ^= 1u << stage;
-        if (!ok) there = 0;
+        if (__all_sync(0xffffffffu, !(ring_state & kGaveUp) && bar_wait(&full[warp][stage], ring_state >> stage & 1u))) {
+          ring_state ^= 1u << stage;
+        } else {
+          ring_state |= kGaveUp;
+          there = 0;
+        }
       }
       // The arithmetic of a step, made with and without masks, as most steps have nothing to mask (selected by a condition in one piece of
       // code, masks were computed in every step), and fine or not
@@ -580,9 +588,9 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
       request(k + NS, stage);
       if (++stage == NS) stage = 0;
     }
-    if (!ok) {                                               // let the copies in flight land (bounded)
+    if (ring_state & kGaveUp) {                              // let the copies in flight land (bounded)
       for (int x = 0; x < NS; ++x)
-        if (have >> x * SUB & ((1u << SUB) - 1)) { bar_wait(&full[warp][x], phases >> x & 1u, 100); phases ^= 1u << x; }
+        if (data_of(x)) bar_wait(&full[warp][x], ring_state >> x & 1u, 100);
       if (lane == 0) atomicExch(c.status, GEAR_ERR_TIMEOUT);
     }
     __syncthreads();                                         // the rings are done with
