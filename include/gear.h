@@ -394,7 +394,9 @@ gear_status gear_fp16_attn_static_status(int32_t* code);
  * residual is not kept.  Nothing faults, traps or hangs. */
 gear_status gear_test_dead_wait(gear_cache* cache, int32_t on);
 /* The same for gear_paged_attn, for the whole process: while `which` is 1, the first warp of every CTA of the kernel of few rows
- * waits once, behind its first requests, on a barrier that nothing completes.  0: off. */
+ * waits once, behind its first requests, on a barrier that nothing completes.  2 to 6: so does, in the kernel of many rows, a warp of
+ * rows, the one that copies keys and values, the one that copies queries, the one that issues products, a warp that converts codes, and every wait
+ * there has that short limit.  0: off. */
 gear_status gear_paged_test_dead_wait(int32_t which);
 
 const char* gear_strerror(gear_status s);

@@ -457,7 +457,7 @@ extern "C" gear_status gear_paged_read(const gear_paged_cache* cache, void* K, v
 }
 
 extern "C" gear_status gear_paged_test_dead_wait(int32_t which) {
-  if (which < 0 || which > 1) return GEAR_ERR_ARG;
+  if (which < 0 || which > 6) return GEAR_ERR_ARG;
   test_dead_wait.store(which, std::memory_order_relaxed);
   return GEAR_OK;
 }
@@ -489,5 +489,6 @@ extern "C" gear_status gear_paged_attn(const gear_paged_cache* cache, const void
   a.causal = causal != 0; a.window = window;
   a.scale_log2 = sc * 1.4426950408889634f;
   a.test_dead_wait = test_dead_wait.load(std::memory_order_relaxed);
+  a.wait_limit = a.test_dead_wait ? kTestSpinLimit : kDecodeSpinLimit;
   return launched(launch_paged_attn(a, cache->bits, cache->dtype, cache->group, scratch, (cudaStream_t)stream));
 }

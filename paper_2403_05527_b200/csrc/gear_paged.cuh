@@ -41,7 +41,8 @@ struct PagedAttnArgs {
   int unit_cap, tile_ctas;
   int tile_new;                 // new rows of a tile: 128 / share
   void* shared_units;           // [tile_ctas] TileShared
-  int test_dead_wait;           // test only: the warp that waits on a barrier that nothing completes (gear_paged_test_dead_wait)
+  int wait_limit;               // polls before a wait of the kernel of many rows gives up
+  int test_dead_wait;           // test only: who waits on a barrier that nothing completes (gear_paged_test_dead_wait)
 };
 
 // What a kernel needs to be told once per device before it is launched there: the shared memory it takes beyond the default.  Calls from

@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(W * 32, MINB) paged_rows_kernel(PagedAttnArgs 
         for (int x = 0; x < D / 32; ++x) qf[n][BITS == 16 ? x : 0] = query(n, x / (kKeyChannels / 8), x % (kKeyChannels / 8));
     }
 
-    if (a.test_dead_wait && warp == 0 && !bar_wait(&dead, 0, kTestSpinLimit)) ring_state |= kGaveUp;
+    if (a.test_dead_wait == 1 && warp == 0 && !bar_wait(&dead, 0, kTestSpinLimit)) ring_state |= kGaveUp;
     int stage = 0;
     for (int k = 0; k < steps_mine; ++k) {
       const int t0 = u.first + (st0 + warp + k * W) * kSpan;

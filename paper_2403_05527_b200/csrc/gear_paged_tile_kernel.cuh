@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
   using S = TileSmem<BITS, D>;
   constexpr int NS = S::kStages;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t kv_full[NS], kv_empty[NS], q_full[2], q_empty[2], s_full[2], p_part[2], p_full[2], pv_done[2], edge;
+  __shared__ uint64_t kv_full[NS], kv_empty[NS], q_full[2], q_empty[2], s_full[2], p_part[2], p_full[2], pv_done[2], edge, ended, dead;
   __shared__ uint64_t raw_full[S::kAhead + 1], raw_empty[S::kAhead + 1];
   __shared__ int2 raw_rows[S::kAhead + 1];
   __shared__ uint32_t tmem_slot;
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
       bar_init(&p_full[t], 4);
     }
     for (int i = 0; i < S::kAhead; ++i) { bar_init(&raw_full[i]); bar_init(&raw_empty[i], kBringWarps<BITS>); }
-    bar_init(&edge);
+    for (uint64_t* b : {&edge, &ended, &dead}) bar_init(b);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kProducts) tmem_alloc<512>(&tmem_slot);
@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
   const bool any = it.f < it.f1;
   if (any) it.find(a);
   bool ok = true;                                            // a wait gave up: go on without waiting, every loop still ends
+  auto test_wait = [&](int who) { if (a.test_dead_wait == who) ok = ok && bar_wait(&dead, 0, kTestSpinLimit); };
 
   // Registers a thread.  A kernel of three or five warpgroups starts with 168 or 96 of them (65536 / 384, / 640, to a multiple of eight);
   // what some warpgroups take, the others have to have given up, else the takers wait for ever.
@@ -133,6 +134,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
     const int heads_q = c.heads * a.share, i_tile = row / a.share, g = row - i_tile * a.share;
     int n_blocks = 0;                                        // of this tile so far
     TileShared shared = {};
+    if (warp == 0) test_wait(2);
     while (any && it.f < it.f1) {
       const int b0 = it.block(), nb = it.blocks_here();
       const int i_unit = it.unit * 2 * a.tile_new, i_first = i_unit + t * a.tile_new, i = i_first + i_tile;
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         const int hi_min = seen_by(p_first, p_first, it.q.len, a.causal, a.window).hi;
         float m = -INFINITY, l = 0.f;
         for (int j = 0; j < nb; ++j) {
-          ok = ok && bar_wait(&s_full[t], (uint32_t)n_blocks & 1u);
+          ok = ok && bar_wait(&s_full[t], (uint32_t)n_blocks & 1u, a.wait_limit);
           tmem_fence_after();
           const int t0 = it.span.first + (b0 + j) * kTileTokens;
           // the arithmetic of a block, made three times: most blocks have nothing to mask (with masks under conditions in one piece of
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
               m = next;
               l *= keep;
               if (j > 0) {                                     // O of the blocks so far; the first product writes over what is there
-                ok = ok && bar_wait(&pv_done[t], (uint32_t)(n_blocks - 1) & 1u);
+                ok = ok && bar_wait(&pv_done[t], (uint32_t)(n_blocks - 1) & 1u, a.wait_limit);
                 tmem_fence_after();
 #pragma unroll 1
                 for (int x = 0; x < D; x += 32) {
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
           ++n_blocks;
         }
         // ---- the unit's result, or this CTA's part of it
-        ok = ok && bar_wait(&pv_done[t], (uint32_t)(n_blocks - 1) & 1u);
+        ok = ok && bar_wait(&pv_done[t], (uint32_t)(n_blocks - 1) & 1u, a.wait_limit);
         tmem_fence_after();
         const bool alone = b0 == 0 && nb == it.span.blocks, wide_out = ((uintptr_t)a.out & 31) == 0;
         float* part = a.partial + ((size_t)blockIdx.x * 2 + (it.unit_at <= (long long)blockIdx.x * per ? 0 : 1)) * kTilePartFloats<D>;
@@ -339,8 +341,10 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         }
       };
       uint32_t st = 0, phase = 0, from = 0, from_phase = 0;
+      if (tp < 32) test_wait(6);
       for (long long left = any ? 2 * (it.f1 - it.f) : 0; left > 0; --left) {
-        ok = ok && bar_wait(&raw_full[from], from_phase) && bar_wait(&kv_empty[st], phase ^ 1u);
+        ok = __all_sync(0xffffffffu, ok && bar_wait(&raw_full[from], from_phase, a.wait_limit) && bar_wait(&kv_empty[st], phase ^ 1u, a.wait_limit));
+        if (!ok) break;                                      // raw_empty may not be told of copies that have not landed
         const unsigned char* src = ahead + from * S::kAheadBytes;
         unsigned char* dst = stages + st * S::kOperand;
         const int2 rows = raw_rows[from];
@@ -354,10 +358,8 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
           // tokens of other rows may have anything there: a step and a minimum of zero stand for zero
           if (row < rows.x || row >= rows.y) par[k] = 0;
         }
-        if (ok) {
 #pragma unroll
-          for (int k = 0; k < kTimes; ++k) convert(dst, k, codes[k], par[k]);
-        }
+        for (int k = 0; k < kTimes; ++k) convert(dst, k, codes[k], par[k]);
         async_fence();
         __syncwarp();
         if (lane == 0) { bar_arrive(&kv_full[st]); bar_arrive(&raw_empty[from]); }
@@ -384,7 +386,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         const bool ragged = t0 < it.span.lo || t0 + kTileTokens > it.span.hi;
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-          ok = __all_sync(0xffffffffu, ok && bar_wait(&kv_empty[st], phase ^ 1u));
+          ok = __all_sync(0xffffffffu, ok && bar_wait(&kv_empty[st], phase ^ 1u, a.wait_limit));
           if (!ok) break;
           unsigned char* dst = stages + st * S::kOperand;
           // values behind the last token or ahead of the first may be no numbers, which a probability of zero does not hide: they
@@ -395,7 +397,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
           __syncwarp();
           if (on) load_page_box(dst + half * S::kHalf + (slot_page << c.page_shift) * 128, &maps.kv[side], half * 64, 0, it.head, page, bar);
           if (fix) {
-            ok = __all_sync(0xffffffffu, bar_wait(&edge, edges++ & 1u));
+            ok = __all_sync(0xffffffffu, bar_wait(&edge, edges++ & 1u, a.wait_limit));
             const int lo = max(0, it.span.lo - t0), hi = max(lo, min(kTileTokens, it.span.hi - t0));
             for (int x = lane; x < kTileTokens * (D / 8); x += 32) {
               const int row = x / (D / 8), p = x % (D / 8);
@@ -408,9 +410,11 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
           ++copies;
           if (++st == NS) { st = 0; phase ^= 1u; }
         }
+        test_wait(3);
       }
-      if (!ok)                                               // let the copies in flight land (bounded)
-        for (int x = max(0, copies - NS); x < copies; ++x) bar_wait(&kv_full[x % NS], (uint32_t)(x / NS) & 1u, 100);
+      // copies land before their memory goes (bounded), whoever gave up
+      if (edges) bar_wait(&edge, (edges - 1) & 1u, 100);
+      for (int x = max(0, copies - NS); x < copies; ++x) bar_wait(&kv_full[x % NS], (uint32_t)(x / NS) & 1u, 100);
     }
     if (BITS != 16 && warp == kProducts + 2) {
       // ============================================================== codes and parameters of a page, a lane each
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, on)) * (code_bytes + param_bytes);
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-          ok = __all_sync(0xffffffffu, ok && bar_wait(&raw_empty[from], phase ^ 1u));
+          ok = __all_sync(0xffffffffu, ok && bar_wait(&raw_empty[from], phase ^ 1u, a.wait_limit));
           if (!ok) break;
           unsigned char* dst = ahead + from * S::kAheadBytes;
           if (lane == 0) {
@@ -444,9 +448,9 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
           ++copies;
           if (++from == S::kAhead) { from = 0; phase ^= 1u; }
         }
+        test_wait(3);
       }
-      if (!ok)                                               // let the copies in flight land (bounded)
-        for (int x = max(0, copies - S::kAhead); x < copies; ++x) bar_wait(&raw_full[x % max(1, S::kAhead)], (uint32_t)(x / max(1, S::kAhead)) & 1u, 100);
+      for (int x = max(0, copies - S::kAhead); x < copies; ++x) bar_wait(&raw_full[x % max(1, S::kAhead)], (uint32_t)(x / max(1, S::kAhead)) & 1u, 100);     // as above
     }
     if (warp == kProducts + 1 && lane == 0) {
       // ============================================================== query rows into their tiles: a box of 64 channels by whole new rows
@@ -456,7 +460,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         for (int t = 0; t < 2 && ok; ++t) {
           const int i_first = (it.unit * 2 + t) * a.tile_new;
           if (i_first >= it.q.rows) break;
-          ok = bar_wait(&q_empty[t], ~units_of[t] & 1u);
+          ok = bar_wait(&q_empty[t], ~units_of[t] & 1u, a.wait_limit);
           if (!ok) break;
           ++units_of[t];
           bar_expect(&q_full[t], bytes);
@@ -465,10 +469,10 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         }
         it.f += it.blocks_here();
         it.settle(a);
+        test_wait(4);
       }
-      if (!ok)                                               // let the copies in flight land (bounded)
-        for (int t = 0; t < 2; ++t)
-          if (units_of[t]) bar_wait(&q_full[t], (units_of[t] - 1) & 1u, 100);
+      for (int t = 0; t < 2; ++t)                            // as above
+        if (units_of[t]) bar_wait(&q_full[t], (units_of[t] - 1) & 1u, 100);
     }
     if (warp == kProducts) {
       // ============================================================== products
@@ -511,7 +515,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
       while (any && ok && it.f < it.f1) {
         const int nb = __shfl_sync(0xffffffffu, it.blocks_here(), 0);
         const bool two = __shfl_sync(0xffffffffu, (it.unit * 2 + 1) * a.tile_new < it.q.rows, 0);
-        auto wait = [&](uint64_t* b, uint32_t parity) { ok = ok && bar_wait(b, parity & 1u); ok = __all_sync(0xffffffffu, ok); tmem_fence_after(); return ok; };
+        auto wait = [&](uint64_t* b, uint32_t parity) { ok = ok && bar_wait(b, parity & 1u, a.wait_limit); ok = __all_sync(0xffffffffu, ok); tmem_fence_after(); return ok; };
         if (!wait(&kv_full[k.st], k.phase) || !wait(&q_full[0], units_of[0]++)) break;
         scores(0, k.st);
         if (nb == 1) release(&q_empty[0]);                   // the tile's next rows may come
@@ -521,6 +525,7 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
           if (nb == 1) release(&q_empty[1]);
         }
         release(&kv_empty[k.st]);
+        test_wait(5);
         for (int j = 0; j < nb; ++j) {
           const Place v = after(k), next = after(v);
           if (!wait(&kv_full[v.st], v.phase) || !wait(kSplit ? &p_part[0] : &p_full[0], blocks_of[0])) break;
@@ -550,6 +555,11 @@ __global__ void __launch_bounds__(kTileThreads<BITS>, 1) paged_tile_kernel(Paged
         }
         it.f += nb;
         it.settle(a);
+      }
+      // products end before their operands' memory and tensor memory go (bounded); whoever reads the last ones may have given up
+      if (any) {
+        release(&ended);
+        bar_wait(&ended, 0, 100);
       }
     }
     __syncwarp();
