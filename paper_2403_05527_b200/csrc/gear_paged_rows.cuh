@@ -141,7 +141,9 @@ template <int SPAN> __device__ __forceinline__ RowsUnit rows_unit(const PagedAtt
 template <int BITS, int D, int NQ, int W> struct RowsRing {
   static constexpr int kRowBytes = D * BITS / 8, kCodes = kStep * kRowBytes, kParams = BITS == 16 ? 0 : kStep * D / 32 * 4;    // of a side
   static constexpr int kPart = 2 * (kCodes + kParams), kStage = kStepParts<BITS> * kPart;
-  static constexpr int kStages = BITS == 16 ? (D == 128 ? 3 : 4) : 2;      // room for two CTAs per SM
+  // Room for two CTAs per SM (one with D = 128 and W = 8).  D = 64 with eight warps: 64 ragged contexts up to 8192, 8 heads, 154 us with four stages,
+  // whose second CTA had no room, now 135 (four warps with four stages 137)
+  static constexpr int kStages = BITS == 16 ? (D == 128 || W == 8 ? 3 : 4) : 2;
   static constexpr int kQPitch = D * 2 + 16, kOPitch = D + 2;
   static constexpr int kRings = W * kStages * kStage, kJoin = W * NQ * 8 * kOPitch * 4;
   static constexpr int kQuery = kRings > kJoin ? kRings : (kJoin + 127) / 128 * 128;         // byte where the query rows begin
@@ -704,6 +706,8 @@ constexpr int kRowsLeastTokens = 256, kRowsSeveral = 8;
 template <class T, int BITS, int D, int NQ, int W, int MINB>
 cudaError_t launch_rows_t(const PagedAttnArgs& a, int group, cudaStream_t st) {
   constexpr int kBytes = RowsRing<BITS, D, NQ, W>::kBytes;
+  // 228 KB per SM, of which each CTA takes 1 KB and less than one for its barriers beside what it asks for
+  static_assert(MINB * (kBytes + 2048) <= 228 * 1024, "MINB CTAs have no room on an SM");
   int shift = 0, sms = 0;
   while ((1 << shift) < group) ++shift;
   static KernelReady ready;
