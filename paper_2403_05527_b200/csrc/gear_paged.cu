@@ -65,6 +65,19 @@ __device__ __forceinline__ int2 place_of_row(const PagedArgs& c, int row) {
   return make_int2(page_of(c, s, t), t & (c.page_size - 1));
 }
 
+// What is wrong with the tables is found by the first CTA, whatever rows look up: a row within the ranges of two sequences finds one of them, and
+// sequences without rows are found by none
+__device__ __forceinline__ void check_tables(const PagedArgs& c) {
+  if (blockIdx.x != 0 || blockIdx.y != 0) return;
+  bool bad = threadIdx.x == 0 && __ldcg(c.row_start) != 0;
+  for (int s = threadIdx.x; s < c.n_seqs; s += kAppendThreads) {
+    const RowRange r = rows_of(c.row_start, s, c.n_rows);
+    const Length n = length_of(c.lengths, s, c.table_stride, c.page_size);
+    bad = bad || r.bad || n.bad || r.hi - r.lo > n.n;
+  }
+  if (bad) paged_bad(c);
+}
+
 // Rows as they are.  Bound: HBM.  A thread takes 16 bytes of a row of K and of V, PER times; the loads of the rows do not wait for the
 // look-up of their slots.
 template <int PER>
@@ -86,6 +99,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(PagedArgs 
       x[j][1] = __ldcg(reinterpret_cast<const uint4*>(v_new + (row0 + r) * v_stride) + rem);
     }
   }
+  check_tables(c);
   for (int r = tid; r < rows; r += kAppendThreads) where[r] = place_of_row(c, row0 + r);
   __syncthreads();
 #pragma unroll
@@ -128,6 +142,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_codes_kernel(Page
   after_previous();
   uint32_t x[16];
   load_32_entries(x, src, r < rows);
+  check_tables(c);
   for (int q = tid; q < rows; q += kAppendThreads) where[q] = place_of_row(c, row0 + q);
 
   uint32_t lo2 = x[0], hi2 = x[0];
