@@ -293,7 +293,7 @@ typedef struct gear_paged_cache {
 #define GEAR_PAGED_SCRATCH_MIN 256
 size_t gear_paged_scratch_bytes(const gear_paged_cache* cache, int64_t n_rows, int32_t n_q_heads);
 gear_status gear_paged_scratch_init(void* scratch, size_t scratch_bytes, void* stream);
-/* Reads and clears the status word; synchronises the device. */
+/* Reads and clears the status word; synchronises the current device, which has to be the scratch's. */
 gear_status gear_paged_status(void* scratch, int32_t* code);
 
 /* Write the new rows of every sequence into their slots, quantized if the cache holds codes.

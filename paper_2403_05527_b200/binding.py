@@ -363,12 +363,19 @@ def gear_paged_scratch_bytes(cache, n_rows: int, n_q_heads: int) -> int:
     return lib().gear_paged_scratch_bytes(cache.ref, n_rows, n_q_heads)
 
 
+def _scratch_here(scratch):
+    if scratch.get_device() != _current_device():
+        raise ValueError("scratch must be on the current device")
+
+
 def gear_paged_scratch_init(scratch, stream=None) -> int:
+    _scratch_here(scratch)
     return _check(lib().gear_paged_scratch_init(_ptr(scratch), scratch.nbytes, _stream(stream)),
                   "gear_paged_scratch_init")
 
 
 def gear_paged_status(scratch) -> int:
+    _scratch_here(scratch)
     code = C.c_int32()
     _check(lib().gear_paged_status(_ptr(scratch), C.byref(code)), "gear_paged_status")
     return code.value
