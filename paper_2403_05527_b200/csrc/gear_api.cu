@@ -1006,8 +1006,9 @@ extern "C" gear_status gear_test_dead_wait(gear_cache* c, int32_t on) {
 extern "C" gear_status gear_fp16_attn_status(void* scratch, int32_t* code) {
   if (!scratch || !code) return GEAR_ERR_ARG;
   int v = 0;
+  // the second wait: a call that follows on a stream which does not wait for the default one may not find the word cleared behind it
   if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&v, scratch, 4, cudaMemcpyDeviceToHost) != cudaSuccess ||
-      cudaMemset(scratch, 0, 4) != cudaSuccess) {
+      cudaMemset(scratch, 0, 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     cudaGetLastError();
     return GEAR_ERR_CUDA;
   }
