@@ -249,15 +249,19 @@ gear_status gear_fp16_decode_attn_static(const void* K, const void* V, const voi
  * when its row is written (Eq. 2, per token, no outliers), in binary32, round to nearest even, without FMA:
  *   m = min x, M = max x;  D = dtype((M - m) * R), R the binary32 nearest to 1 / (2^b - 1), or 0 where that is below 2^-126;
  *   code = clamp(rint((x - m) * (1 / D)), 0, 2^b - 1), or 0 where D = 0
- * and stands for dtype(code * D + m).  Two 4-bit codes share a byte, the even channel in the low half.
- * Rows are assumed finite, of magnitude below 2^126; what lies in slots behind a sequence's last token, in pages that no
+ * and stands for dtype(code * D + m).  (gear_paged_read, and gear_paged_attn over 8-bit codes of bf16, round the sum to binary32
+ * first and then to dtype, gear_paged_attn over other codes once: where the sum is inexact in binary32 and lies half way between two values
+ * of dtype there, the two differ by one unit in the last place.)  Two 4-bit codes share a byte, the even channel in the low half.
+ * Rows are assumed finite, of magnitude below 2^126, and so is what their codes stand for (in fp16 a step that is rounded up can take the
+ * last code of a group that spans nearly all of the type past its largest number); what lies in slots behind a sequence's last token, in pages that no
  * sequence uses and in slots that a window has passed may be anything.
  *
  * Token t of sequence s lies in slot t % page_size of page page_table[s * table_stride + t / page_size].  lengths[s] counts the tokens of
  * sequence s INCLUDING the rows that a call brings: the caller adds them before gear_paged_append and leaves the numbers as
  * they are for gear_paged_attn.  Rows of all sequences lie one after the other: sequence s has the rows row_start[s] ..
- * row_start[s + 1] - 1, which are its last tokens, and rows from row_start[n_seqs] on belong to nobody (a padded batch; they are
- * neither read nor written).  Sequences may have no rows and no tokens.
+ * row_start[s + 1] - 1, which are its last tokens, and rows from row_start[n_seqs] on belong to nobody (a padded batch: they may hold
+ * anything, change nothing and are not written, but all n_rows rows have to be memory that can be read).  Sequences may have no
+ * rows and no tokens.
  *
  * Tables are read on the device, so what is wrong with them is found there: a page number outside the pool where a page is needed, a
  * length beyond the table or rows that do not fit (row_start that falls or passes n_rows; more rows than max_rows or

@@ -7,7 +7,7 @@
 // multiply-add of 16 bits: the rounding that the cache's definition has).  A warp walks through 16-token steps, which come into a ring of
 // its own in shared memory by bulk copies (a lane each for keys, values and their parameters), several steps ahead; the warps of a CTA
 // take turns.  (With the next step's loads held in registers instead, 16-bit rows waited for memory, 64 ragged contexts up to 8192 168 us,
-// now 133, 87 % of the copy bandwidth; and codes spent 616 instructions per 16 tokens, half of them on addresses, 12 contexts of 32768 in 4
+// now 134, 86 % of the copy bandwidth; and codes spent 616 instructions per 16 tokens, half of them on addresses, 12 contexts of 32768 in 4
 // bits 161 us, now 428 and 129, bound by the issue of instructions and by their latency at 16 warps per SM.)
 //
 // Work: where there are few (sequence, kv head) units for the CTAs, each is cut evenly into parts of its own, a CTA each; else the steps of
