@@ -36,3 +36,29 @@ def test_many_rows_do_not_depend_on_neighbours(heads, q_heads, bits, group):
         assert max(e) <= 1.0, e
     for out, lse in runs[1:]:
         assert H.same_bits(out, runs[0][0]) and H.same_bits(lse, runs[0][1])
+
+
+@pytest.mark.parametrize("bits,group", [(16, 0), (8, 64), (4, 32)])
+def test_few_rows_do_not_depend_on_neighbours(bits, group):
+    import torch
+    from paper_2403_05527_b200 import binding as G
+    from tests import paged_harness as H
+    lengths, rows, pad = [1500, 700, 90], [2, 3, 1], 5
+    pool = H.Pool(G, lengths, rows, "fp16", bits, group, 16, 2, 128, seed=bits)
+    sides = [[pool.draw(n) for n in lengths] for _ in range(2)]
+    pool.fill(sides)
+    n = pool.n_rows
+    base = (torch.randn((n + pad, 6, 128), generator=pool.gen) * 0.3).to(pool.dtype)
+    scratch = pool.scratch(G, 6, n + pad)
+    runs = []
+    for neighbour, nobody in ((1.0, 1.0), (30.0, 1.0), (30.0, float("nan"))):
+        q = base.clone()
+        q[rows[0]:n] *= neighbour
+        q[n:] *= nobody
+        out, lse = torch.full_like(q, 7.0).cuda(), torch.zeros((n + pad, 6), device="cuda")
+        G.gear_paged_attn(pool.cache, q.cuda(), out, pool.d_starts, scratch, max_rows=3, lse=lse)
+        assert G.gear_paged_status(scratch) == 0
+        assert (out[n:] == 7.0).all() and (lse[n:] == 0.0).all()
+        runs.append((out[:rows[0]].cpu(), lse[:rows[0]].cpu()))
+    for out, lse in runs[1:]:
+        assert H.same_bits(out, runs[0][0]) and H.same_bits(lse, runs[0][1])
